@@ -199,6 +199,9 @@ int dssp_step_done(dssp_ctx* ctx, int worker, int* done_out, int64_t* t_start_us
  *   momentum             in [0, 1);  nesterov 0 / 1;  steps in [1, 64];  eps > 0
  *   momentum_dev         n_params floats, caller-owned, zeroed by the caller before the first push, updated in place by pushes
  *   workspace_dev        dssp_orthogonal_workspace_bytes(...) bytes, 256-byte aligned, caller-owned; contents undefined between calls
+ * A push that this rule cannot take is refused (DSSP_EHIP) before anything is launched: a snapshot that is not 16-byte aligned, gradients or snapshots that overlap the
+ * weights, momentum or workspace, or a snapshot another one or a gradient still to be applied.  Should the device refuse a launch in the middle of an update, the call is not
+ * counted either, but weights and momentum are then undefined.
  * momentum_dev == NULL goes back to the paper's rule.  Waits for the context's earlier pushes.  Buffers must stay until then or until dssp_destroy.
  * dssp_orthogonal_workspace_bytes returns 0 where the matrices are refused; a model's are the segments of kind 0 of dssp_model_segments, fan_in x size / fan_in. */
 size_t dssp_orthogonal_workspace_bytes(const int64_t* offset, const int32_t* rows, const int32_t* cols, int count);

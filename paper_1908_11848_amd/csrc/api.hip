@@ -46,6 +46,7 @@ struct dssp_ctx {
     std::vector<uint8_t> own_wstream;
     hipEvent_t ev_apply = nullptr;                // last apply finished
     hipStream_t apply_stream = nullptr;           // where it was enqueued (what follows on that stream needs no wait); null: not known
+    bool apply_enqueued = false;                  // ev_apply stands for something
     std::vector<hipEvent_t> ev_grad;              // worker's gradient is complete
     std::vector<hipEvent_t> ev_pull;              // worker's snapshot copy finished reading w
     std::vector<uint8_t> pull_pending;            // a pull was enqueued since the last apply
@@ -318,7 +319,7 @@ extern "C" int dssp_pull(dssp_ctx* c, int worker, float* dst_dev, uint64_t* vers
     if (!dst_dev) return fail(c, DSSP_EINVAL, "dst_dev is null");
     if (int rc = ensure_stream(c, worker)) return rc;
     hipStream_t s = c->wstream[worker];
-    if (c->version > 0 && c->apply_stream != s) HIP_TRY(c, hipStreamWaitEvent(s, c->ev_apply, 0));
+    if (c->apply_enqueued && c->apply_stream != s) HIP_TRY(c, hipStreamWaitEvent(s, c->ev_apply, 0));
     if (int rc = dsspk_pull(s, dst_dev, c->params, c->n_params, c->stamps_dev + 1 + worker, c->stamps_dev))
         return fail(c, DSSP_EHIP, "pull kernel launch failed (rc " + std::to_string(rc) + ")");
     HIP_TRY(c, hipEventRecord(c->ev_pull[worker], s));
@@ -437,8 +438,8 @@ Decision decide(dssp_ctx* c, int p, int64_t t_push, int* released) {
 // Stream `as` waits for the apply before it and for every snapshot copy still reading w.  A wait costs the host 2 to 4 us, so
 // none is enqueued for what the stream order, or another of these waits, guarantees: the apply before it on the same
 // stream, and one that a snapshot copy waited for here followed on its stream.
-int wait_for_w(dssp_ctx* c, hipStream_t as, uint64_t applies_before) {
-    bool behind_apply = applies_before == 0 || c->apply_stream == as;
+int wait_for_w(dssp_ctx* c, hipStream_t as) {
+    bool behind_apply = !c->apply_enqueued || c->apply_stream == as;
     for (int q = 0; q < c->K; ++q)
         if (c->pull_pending[q]) {
             if (c->wstream[q] != as) {
@@ -449,6 +450,36 @@ int wait_for_w(dssp_ctx* c, hipStream_t as, uint64_t applies_before) {
         }
     if (!behind_apply) HIP_TRY(c, hipStreamWaitEvent(as, c->ev_apply, 0));
     return DSSP_OK;
+}
+
+// What is on stream `as` now is the last apply: later ones and pulls wait for it.
+int close_apply(dssp_ctx* c, hipStream_t as) {
+    c->apply_stream = as;
+    c->apply_enqueued = true;
+    HIP_TRY(c, hipEventRecord(c->ev_apply, as));
+    return DSSP_OK;
+}
+
+// The update of the orthogonalised rule is many launches and its snapshots are more, where the paper's rule has one that refuses or does everything: whatever of
+// a push these would refuse is refused here, in front of the first of them.  Snapshot e is taken after gradient after[e] (1 .. m).
+const char* orthogonal_refuses(const dssp_ctx* c, int m, const float* const* grads, int n_snap, float* const* dst, const int* after) {
+    auto overlap = [&](const float* a, const void* b, size_t b_bytes) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+        return x < y + b_bytes && y < x + sizeof(float) * (size_t)c->n_params;
+    };
+    const size_t bytes = sizeof(float) * (size_t)c->n_params;
+    auto owned = [&](const float* p) { return overlap(p, c->params, bytes) || overlap(p, c->momentum_dev, bytes) || overlap(p, c->orth_workspace, c->orth_workspace_bytes); };
+    for (int j = 0; j < m; ++j)
+        if (owned(grads[j])) return "a gradient overlaps the weights, the momentum or the workspace";
+    for (int e = 0; e < n_snap; ++e) {
+        if (c->n_params > 3 && ((reinterpret_cast<uintptr_t>(dst[e]) | reinterpret_cast<uintptr_t>(c->params)) & 15)) return "a snapshot or the weights are not 16-byte aligned";
+        if (owned(dst[e])) return "a snapshot overlaps the weights, the momentum or the workspace";
+        for (int f = 0; f < e; ++f)
+            if (overlap(dst[e], dst[f], bytes)) return "two snapshots overlap";
+        for (int j = after[e]; j < m; ++j)
+            if (overlap(dst[e], grads[j], bytes)) return "a snapshot overlaps a gradient that is applied after it";
+    }
+    return nullptr;
 }
 
 // Server step 2 for one gradient under the orthogonalised rule, and the stamp.  Applies of a context follow one another, so they share one workspace.
@@ -464,14 +495,18 @@ int enqueue_orthogonal(dssp_ctx* c, hipStream_t as, const float* grad_dev, uint6
 // snapshot still reading w.  Without a server stream it goes onto the pusher's own stream, right behind the gradient:
 // a separate stream shares a hardware queue with some worker's stream, and the small apply then waits for that
 // worker's whole iteration.
-int enqueue_apply(dssp_ctx* c, int p, const float* grad_dev, float* pull_dst_dev, bool fused, uint64_t applies_before) {
+int enqueue_apply(dssp_ctx* c, int p, const float* grad_dev, float* pull_dst_dev, bool fused) {
+    if (c->momentum_dev) {
+        const int after = 1;
+        if (const char* why = orthogonal_refuses(c, 1, &grad_dev, fused ? 1 : 0, &pull_dst_dev, &after)) return fail(c, DSSP_EHIP, why);
+    }
     const bool own = c->server_stream == nullptr;
     hipStream_t as = own ? c->wstream[p] : c->server_stream;
     if (!own) {
         HIP_TRY(c, hipEventRecord(c->ev_grad[p], c->wstream[p]));
         HIP_TRY(c, hipStreamWaitEvent(as, c->ev_grad[p], 0));
     }
-    if (int rc = wait_for_w(c, as, applies_before)) return rc;
+    if (int rc = wait_for_w(c, as)) return rc;
     int rc;
     if (c->momentum_dev) {
         rc = enqueue_orthogonal(c, as, grad_dev, c->version);
@@ -481,9 +516,11 @@ int enqueue_apply(dssp_ctx* c, int p, const float* grad_dev, float* pull_dst_dev
                               c->stamps_dev + 1 + p, c->version);
     else
         rc = dsspk_apply(as, c->params, grad_dev, c->n_params, c->scale, c->stamps_dev, c->version);
-    if (rc) return fail(c, DSSP_EHIP, "apply kernel launch failed (rc " + std::to_string(rc) + ")");
-    HIP_TRY(c, hipEventRecord(c->ev_apply, as));
-    c->apply_stream = as;
+    if (rc) {
+        if (c->momentum_dev) (void)close_apply(c, as);      // a part of the update may be on its way: later work stays behind it
+        return fail(c, DSSP_EHIP, "apply kernel launch failed (rc " + std::to_string(rc) + ")");
+    }
+    if (int rcc = close_apply(c, as)) return rcc;
     if (fused && !own) HIP_TRY(c, hipStreamWaitEvent(c->wstream[p], c->ev_apply, 0));
     return DSSP_OK;
 }
@@ -507,7 +544,7 @@ int push_impl(dssp_ctx* c, int worker, const float* grad_dev, int64_t t_push, fl
     const Decision d = decide(c, p, t_push, released_out);
     const bool fused = d.ok && pull_dst_dev != nullptr;
     if (!c->host_only)
-        if (int rc = enqueue_apply(c, p, grad_dev, pull_dst_dev, fused, before.version)) {
+        if (int rc = enqueue_apply(c, p, grad_dev, pull_dst_dev, fused)) {
             restore_state(c, before);       // nothing of this push counts: the caller may repeat it or give up
             return rc;
         }
@@ -587,6 +624,13 @@ extern "C" int dssp_push_many(dssp_ctx* c, int m, const int* workers, const floa
     auto undo = [&](int rc) { restore_state(c, before); return rc; };
     const bool own = c->server_stream == nullptr;
     hipStream_t as = own ? c->wstream[workers[0]] : c->server_stream;
+    float* dst[DSSPK_APPLY_MANY_MAX_DST];
+    for (int e = 0; e < n_snap; ++e) {
+        dst[e] = pull_dst_dev[snap_worker[e]];
+        if (!dst[e]) return undo(fail(c, DSSP_EINVAL, "pull_dst_dev of a worker that may go on is null"));
+    }
+    if (c->momentum_dev)
+        if (const char* why = orthogonal_refuses(c, m, grads_dev, n_snap, dst, snap_after)) return undo(fail(c, DSSP_EHIP, why));
     // Workers may share a stream; one event says that all gradients on it are complete, one wait holds up all of its workers (with an event
     // and a wait each, 16 pushers on four streams left the GPU 120 us between two aggregated applies of 25 M parameters, 631 us each).
     auto shares = [&](const int* list, int k) {     // the stream of list[k] with one listed before
@@ -600,12 +644,9 @@ extern "C" int dssp_push_many(dssp_ctx* c, int m, const int* workers, const floa
         if (hipEventRecord(c->ev_grad[workers[j]], ws) != hipSuccess || hipStreamWaitEvent(as, c->ev_grad[workers[j]], 0) != hipSuccess)
             return undo(fail(c, DSSP_EHIP, "event between a pusher's stream and the apply's"));
     }
-    if (int rc = wait_for_w(c, as, before.version)) return undo(rc);
-    float* dst[DSSPK_APPLY_MANY_MAX_DST];
+    if (int rc = wait_for_w(c, as)) return undo(rc);
     uint64_t* dst_stamp[DSSPK_APPLY_MANY_MAX_DST];
     for (int e = 0; e < n_snap; ++e) {
-        dst[e] = pull_dst_dev[snap_worker[e]];
-        if (!dst[e]) return undo(fail(c, DSSP_EINVAL, "pull_dst_dev of a worker that may go on is null"));
         if (int rc = ensure_stream(c, snap_worker[e])) return undo(rc);
         dst_stamp[e] = c->stamps_dev + 1 + snap_worker[e];
     }
@@ -615,12 +656,14 @@ extern "C" int dssp_push_many(dssp_ctx* c, int m, const int* workers, const floa
             rc = enqueue_orthogonal(c, as, grads_dev[j], before.version + 1 + j);
             for (; e < n_snap && snap_after[e] == j + 1 && !rc; ++e) rc = dsspk_pull(as, dst[e], c->params, c->n_params, dst_stamp[e], c->stamps_dev);
         }
-        if (rc) return undo(fail(c, DSSP_EHIP, "orthogonalised apply: launch failed (rc " + std::to_string(rc) + ")"));
+        if (rc) {
+            (void)close_apply(c, as);           // as in enqueue_apply
+            return undo(fail(c, DSSP_EHIP, "orthogonalised apply: launch failed (rc " + std::to_string(rc) + ")"));
+        }
     } else if (int rc = dsspk_apply_many(as, c->params, m, grads_dev, c->n_params, c->scale, n_snap, dst, snap_after, dst_stamp, c->stamps_dev,
                                   before.version + 1))
         return undo(fail(c, DSSP_EHIP, "aggregated apply kernel launch failed (rc " + std::to_string(rc) + ")"));
-    HIP_TRY(c, hipEventRecord(c->ev_apply, as));
-    c->apply_stream = as;
+    if (int rc = close_apply(c, as)) return rc;
     for (int e = 0; e < n_snap; ++e)        // whoever got a snapshot goes on behind the kernel that wrote it
         if (c->wstream[snap_worker[e]] != as && !shares(snap_worker, e)) HIP_TRY(c, hipStreamWaitEvent(c->wstream[snap_worker[e]], c->ev_apply, 0));
     return DSSP_OK;
