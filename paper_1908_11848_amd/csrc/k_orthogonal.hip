@@ -657,10 +657,12 @@ __global__ __launch_bounds__(SMALL_THREADS, 4) void small_kernel(Group grp, char
 
 // ---------------------------------------------------------------- host
 
+constexpr int64_t MAX_ENTRIES = 1LL << 38;
 bool bad(const dsspk_matrix* m, int count) {
     if (count < 0 || (count && !m)) return true;
     int64_t steps = 0;
     for (int i = 0; i < count; ++i) {
+        if (m[i].offset > MAX_ENTRIES) return true;          // (behind which an offset's sums might not fit 64 bits)
         if (m[i].rows < 1 || m[i].cols < 1 || m[i].rows > 1 << 20 || m[i].cols > 1 << 20 || (int64_t)m[i].rows * m[i].cols > 1LL << 31 || m[i].offset < 0) return true;
         if ((m[i].rows < m[i].cols ? m[i].rows : m[i].cols) > 1 << 14) return true;
         const Room r(m[i].rows, m[i].cols);
@@ -721,7 +723,7 @@ extern "C" size_t dsspk_orthogonal_workspace_bytes(const dsspk_matrix* matrices,
 extern "C" int dsspk_orthogonal_apply(void* stream, const float* w, float* w_out, const float* m, float* m_out, const float* g, int64_t n, const dsspk_matrix* matrices,
                                       int count, float scale, float rest_scale, float momentum, int nesterov, int steps, float eps, void* workspace,
                                       size_t workspace_bytes) {
-    if (bad(matrices, count) || !w || !w_out || !m || !m_out || !g || n < 0 || n > 1LL << 38 || steps < 1 || steps > 64 || !(eps > 0.f)) return -1;
+    if (bad(matrices, count) || !w || !w_out || !m || !m_out || !g || n < 0 || n > MAX_ENTRIES || steps < 1 || steps > 64 || !(eps > 0.f)) return -1;
     if (count && matrices[count - 1].offset + (int64_t)matrices[count - 1].rows * matrices[count - 1].cols > n) return -1;
     if (w_out == g || m_out == g || w_out == m || m_out == w || w_out == m_out) return -1;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < dsspk_orthogonal_workspace_bytes(matrices, count)) return -1;

@@ -37,3 +37,13 @@ def test_host_only_context_has_no_rule():
         B.dssp_set_orthogonal_update(ctx, [(0, 2, 2)], 0.1, 16, 256, 1 << 20)
     assert e.value.code == B.DSSP_ESTATE
     B.dssp_destroy(ctx)
+
+
+@pytest.mark.parametrize("matrices", [[(2 ** 63 - 1, 3, 3)], [(2 ** 63 - 9, 3, 3)], [(0, 2, 2), (2 ** 63 - 8, 3, 3)], [(2 ** 63 - 9, 3, 3), (5, 3, 3)]])
+def test_matrices_whose_end_passes_64_bits_are_refused(matrices):
+    """offset + rows * cols wraps round and would look as if it were within the vector"""
+    assert B.dssp_orthogonal_workspace_bytes(matrices) == 0
+    table = B.matrix_table(matrices)
+    assert B.lib().dsspk_orthogonal_workspace_bytes(table, len(matrices)) == 0
+    # refused by its arguments, in front of any launch (the addresses are never used)
+    assert B.lib().dsspk_orthogonal_apply(None, 1 << 20, 2 << 20, 3 << 20, 4 << 20, 5 << 20, 100, table, len(matrices), 0.1, 0.1, 0.9, 1, 5, 1e-7, 6 << 20, 1 << 60) == -1
