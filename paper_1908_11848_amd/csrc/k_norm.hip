@@ -216,8 +216,12 @@ int records_of(int64_t M, int C) {
 
 template <class T, int E, int WAVES, int ROWS>
 void launch_fwd(hipStream_t s, const void* x, const float* gamma, const float* beta, void* y, float* stats, long ldx, long ldy, long M, int C, float eps) {
-    hipLaunchKernelGGL((layernorm_fwd_kernel<T, E, WAVES, ROWS>), dim3(ceil_div(M, ROWS)), dim3(64 * WAVES * ROWS), 0, s, (const T*)x, gamma, beta, (T*)y, stats,
-                       ldx, ldy, M, C, eps, rows::past_the_caches(M * C * (int64_t)sizeof(T)));
+    const long most = most_blocks(64 * WAVES * ROWS) * ROWS;        // rows of a launch
+    for (long at = 0; at < M; at += most) {
+        const long n = M - at < most ? M - at : most;
+        hipLaunchKernelGGL((layernorm_fwd_kernel<T, E, WAVES, ROWS>), dim3(ceil_div(n, ROWS)), dim3(64 * WAVES * ROWS), 0, s, (const T*)x + at * ldx, gamma, beta,
+                           (T*)y + at * ldy, stats ? stats + 2 * at : nullptr, ldx, ldy, n, C, eps, rows::past_the_caches(M * C * (int64_t)sizeof(T)));
+    }
 }
 template <class T, int E, int WAVES, int ROWS>
 void launch_bwd(hipStream_t s, int G, const void* x, const float* gamma, const float* stats, const void* dy, const void* add, void* dx, float* dgamma,
