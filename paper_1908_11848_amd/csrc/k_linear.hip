@@ -27,16 +27,16 @@ struct Pack {
     int cols, padded;       // columns, rounded up to 8 (bf16) or 32 (fp32)
     long first_block;
 };
-struct Packs { Pack p[3]; int count; };
+struct Packs { Pack p[3]; int count; long base; };      // base: blocks of the launches before
 
 constexpr int PACK_THREADS = 256;
 // a lane writes 8 elements of each plane
 template <class T> __global__ __launch_bounds__(PACK_THREADS) void pack_kernel(Packs packs) {
     int j = 0;
     for (int i = 1; i < packs.count; ++i)
-        if ((long)blockIdx.x >= packs.p[i].first_block) j = i;
+        if (packs.base + blockIdx.x >= packs.p[i].first_block) j = i;
     const Pack& p = packs.p[j];
-    const long at = ((long)blockIdx.x - p.first_block) * PACK_THREADS + threadIdx.x;
+    const long at = (packs.base + blockIdx.x - p.first_block) * PACK_THREADS + threadIdx.x;
     const int chunks = p.padded / 8;
     const long row = at / chunks;
     const int col = (int)(at - row * chunks) * 8;
@@ -333,8 +333,7 @@ int slabs_of(int64_t M, int N) {            // some 1024 workgroups, 16 rows a s
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(float* p, long n) {
-    const long at = (long)blockIdx.x * 256 + threadIdx.x;
-    if (at < n) p[at] = 0.f;
+    for (long at = (long)blockIdx.x * 256 + threadIdx.x; at < n; at += (long)gridDim.x * 256) p[at] = 0.f;
 }
 
 __global__ __launch_bounds__(256) void to_bf16_kernel(bf16* __restrict__ dst, const float* __restrict__ src, long n) {
@@ -359,10 +358,17 @@ inline size_t pack_bytes(int type, int64_t rows, int64_t cols) { return round256
 // all operand orders alike within 5 %): a step of BK indices with one workgroup on a compute unit and with all it holds, what a tile costs besides its steps, and partial
 // sums that are written and read at 4 TB/s behind another launch.
 struct Choice { int tile, parts; };
-struct Cost { int bm, bn, bk, fit; float alone, full, more; };
+struct Cost { int bm, bn, bk, threads, fit; float alone, full, more; };
 constexpr int TILES = 3;
-constexpr Cost COSTS[2][TILES] = {{{128, 64, 32, 2, 0.75f, 1.27f, 3.f}, {128, 128, 32, 1, 0.88f, 1.11f, 3.f}, {64, 64, 32, 1, 0.46f, 0.48f, 3.f}},         // fp32
-                                  {{128, 128, 64, 2, 0.68f, 0.99f, 3.f}, {256, 256, 64, 1, 1.40f, 1.56f, 4.f}}};                                          // bf16 (none)
+constexpr Cost COSTS[2][TILES] = {{{128, 64, 32, 256, 2, 0.75f, 1.27f, 3.f}, {128, 128, 32, 512, 1, 0.88f, 1.11f, 3.f}, {64, 64, 32, 256, 1, 0.46f, 0.48f, 3.f}},      // fp32
+                                  {{128, 128, 64, 256, 2, 0.68f, 0.99f, 3.f}, {256, 256, 64, 512, 1, 1.40f, 1.56f, 4.f}}};                                          // bf16 (none)
+inline int64_t tiles_of(const Cost& c, int64_t rows, int64_t cols) { return ((rows + c.bm - 1) / c.bm) * ((cols + c.bn - 1) / c.bn); }
+// whether there is a tile for a result of that size: one launch has all of its tiles
+inline bool launchable(int type, int64_t rows, int64_t cols) {
+    for (const Cost& c : COSTS[type == DSSPK_BF16])
+        if (c.bm && tiles_of(c, rows, cols) <= most_blocks(c.threads)) return true;
+    return false;
+}
 constexpr int CUS = 256, MAX_PARTS = 64;
 Choice choose(int type, int64_t rows, int64_t cols, int64_t K) {
     Choice best = {0, 1};
@@ -370,8 +376,10 @@ Choice choose(int type, int64_t rows, int64_t cols, int64_t K) {
     for (int tile = 0; tile < TILES; ++tile) {
         const Cost& c = COSTS[type == DSSPK_BF16][tile];
         if (!c.bm) continue;
-        const int64_t tiles = ((rows + c.bm - 1) / c.bm) * ((cols + c.bn - 1) / c.bn), steps = (K + c.bk - 1) / c.bk;
-        for (int parts = 1; parts <= MAX_PARTS && (parts == 1 || steps / parts >= 4); ++parts) {
+        const int64_t tiles = tiles_of(c, rows, cols), steps = (K + c.bk - 1) / c.bk;
+        if (tiles > most_blocks(c.threads)) continue;
+        // (what is split has few tiles: so many that their parts or their join would not fit a launch are never worth it)
+        for (int parts = 1; parts <= MAX_PARTS && (parts == 1 || (steps / parts >= 4 && tiles * parts <= 1 << 20)); ++parts) {
             const int64_t n = tiles * parts, each = (steps + parts - 1) / parts, slots = (int64_t)CUS * c.fit;
             const int64_t full = n / slots, rest = n - full * slots;
             float t = full * (each * c.full + c.more);
@@ -417,15 +425,18 @@ int pack(hipStream_t s, int type, int n, const Matrix* m, Source* out, char*& ws
         const int64_t cols = padded(type, m[i].cols);
         Pack& p = packs.p[packs.count++];
         p = {m[i].p, ws, m[i].ld, m[i].rows, m[i].cols, (int)cols, blocks};
-        blocks += ceil_div(m[i].rows * (cols / 8), PACK_THREADS);
+        blocks += (m[i].rows * (cols / 8) + PACK_THREADS - 1) / PACK_THREADS;
         out[i].p = ws;
         out[i].pitch = type == DSSPK_F32 ? prod::terms_pitch(cols) : 2 * cols;
         out[i].cols = cols;
         ws += pack_bytes(type, m[i].rows, m[i].cols);
     }
     if (!packs.count) return 0;
-    if (type == DSSPK_F32) hipLaunchKernelGGL((pack_kernel<float>), dim3(blocks), dim3(PACK_THREADS), 0, s, packs);
-    else hipLaunchKernelGGL((pack_kernel<bf16>), dim3(blocks), dim3(PACK_THREADS), 0, s, packs);
+    for (const long most = most_blocks(PACK_THREADS); packs.base < blocks; packs.base += most) {
+        const dim3 grid(blocks - packs.base < most ? blocks - packs.base : most);
+        if (type == DSSPK_F32) hipLaunchKernelGGL((pack_kernel<float>), grid, dim3(PACK_THREADS), 0, s, packs);
+        else hipLaunchKernelGGL((pack_kernel<bf16>), grid, dim3(PACK_THREADS), 0, s, packs);
+    }
     return DSSPK_LAUNCH_RC();
 }
 
@@ -491,9 +502,8 @@ template <class T> int few_rows(hipStream_t s, const void* x, int64_t ldx, const
 bool bad(int type, int64_t M, int N, int K) {
     return (type != DSSPK_F32 && type != DSSPK_BF16) || M < 0 || M > MAX_ROWS || N < 1 || K < 1 || N > MAX_COLS || K > MAX_COLS;
 }
-// a tile's rows times the pitch, and the workgroups of a launch, have to fit 31 bits
+// a tile's rows times the pitch have to fit 31 bits
 inline bool wide(int64_t ld) { return ld > 1L << 21; }
-inline bool many(int64_t M, int64_t cols) { return (M / 64 + 1) * (cols / 64 + 1) >= 1L << 31 || M * ((cols + 31) / 8) / PACK_THREADS >= (1L << 31) - 1; }
 
 }  // namespace
 
@@ -506,7 +516,7 @@ extern "C" int dsspk_linear_fwd(void* stream, int type, const void* x, int64_t l
                                 void* y, int64_t ldy, void* z, int64_t ldz, int64_t M, int N, int K, void* workspace, size_t workspace_bytes) {
     if (bad(type, M, N, K) || !x || !w || !y || ldx < K || ldy < N || (residual && ldr < N) || (z && ldz < N) || act < DSSPK_ACT_NONE || act > DSSPK_ACT_SILU) return -1;
     if (y == x || z == x || y == w || (z && z == y) || (residual == y && ldr != ldy) || (z && z == residual)) return -1;
-    if (wide(ldx) || (residual && wide(ldr)) || many(M, N) || many(M, K)) return -1;
+    if (wide(ldx) || (residual && wide(ldr)) || !launchable(type, M, N)) return -1;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < dsspk_linear_fwd_workspace_bytes(type, M, N, K)) return -1;
     if (M == 0) return 0;
     const hipStream_t s = (hipStream_t)stream;
@@ -540,7 +550,7 @@ extern "C" int dsspk_linear_bwd(void* stream, int type, const void* x, int64_t l
                                 const void* pre, int64_t ldpre, int act, float* dw, float* db, int64_t M, int N, int K, void* workspace, size_t workspace_bytes) {
     if (bad(type, M, N, K) || !dz || lddz < N || (dw && (!x || ldx < K)) || (dx && (!w || lddx < K)) || (pre && (!dx || ldpre < K))) return -1;
     if (act < DSSPK_ACT_NONE || act > DSSPK_ACT_SILU || (!dx && !dw && !db)) return -1;
-    if ((dx && (dx == dz || dx == x || dx == w || dx == pre)) || wide(lddz) || (dw && wide(ldx)) || (pre && wide(ldpre)) || many(M, N) || many(M, K)) return -1;
+    if ((dx && (dx == dz || dx == x || dx == w || dx == pre)) || wide(lddz) || (dw && wide(ldx)) || (pre && wide(ldpre)) || (dx && !launchable(type, M, K)) || (dw && !launchable(type, K, N))) return -1;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < dsspk_linear_bwd_workspace_bytes(type, M, N, K)) return -1;
     const hipStream_t s = (hipStream_t)stream;
     char* ws = (char*)workspace;
@@ -556,7 +566,8 @@ extern "C" int dsspk_linear_bwd(void* stream, int type, const void* x, int64_t l
         if (const int rc = DSSPK_LAUNCH_RC()) return rc;
     }
     if (M == 0 && dw) {
-        hipLaunchKernelGGL(zero_kernel, dim3(ceil_div((long)K * N, 256)), dim3(256), 0, s, dw, (long)K * N);
+        const long n = (long)K * N, blocks = (n + 255) / 256, most = most_blocks(256);
+        hipLaunchKernelGGL(zero_kernel, dim3(blocks < most ? blocks : most), dim3(256), 0, s, dw, n);
         return DSSPK_LAUNCH_RC();
     }
     if (M == 0 || (!dx && !dw)) return 0;
@@ -587,6 +598,10 @@ extern "C" int dsspk_linear_bwd(void* stream, int type, const void* x, int64_t l
 extern "C" int dsspk_to_bf16(void* stream, void* dst, const float* src, int64_t n) {
     if (!dst || (!src && n) || n < 0 || (const void*)dst == (const void*)src || n > (1L << 40)) return -1;
     if (n == 0) return 0;
-    hipLaunchKernelGGL(to_bf16_kernel, dim3(ceil_div(n, 2048)), dim3(256), 0, (hipStream_t)stream, (bf16*)dst, src, (long)n);
+    const int64_t most = most_blocks(256) * 2048;        // of a launch
+    for (int64_t at = 0; at < n; at += most) {
+        const int64_t m = n - at < most ? n - at : most;
+        hipLaunchKernelGGL(to_bf16_kernel, dim3(ceil_div(m, 2048)), dim3(256), 0, (hipStream_t)stream, (bf16*)dst + at, src + at, (long)m);
+    }
     return DSSPK_LAUNCH_RC();
 }

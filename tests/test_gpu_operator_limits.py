@@ -29,3 +29,53 @@ def test_layer_norm_of_more_rows_than_a_launch_has_wavefronts():
         assert L.dsspk_layernorm_fwd(stream(), B.DSSPK_BF16, p(x[at:]), C, p(gamma), p(beta), p(part[at:]), C, p(some[at:]), n, C, 1e-5) == 0
     torch.cuda.synchronize()
     assert torch.equal(y, part) and torch.equal(stats, some) and torch.isfinite(y).all()
+
+
+def needs(nbytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nbytes + (4 << 30):
+        pytest.skip("needs %d GB of device memory" % (nbytes >> 30))
+
+
+def test_weight_gradient_of_no_rows_beyond_32_bits():
+    K, N = 1 << 16, (1 << 16) + 3
+    L = B.lib()
+    nws = L.dsspk_linear_bwd_workspace_bytes(B.DSSPK_BF16, 0, N, K)
+    needs(4 * K * N + nws)
+    dw, ws, some = torch.full((K, N), float("nan"), device="cuda"), torch.empty(nws, dtype=torch.uint8, device="cuda"), torch.empty(8, device="cuda")
+    p = lambda t: t.data_ptr()      # noqa: E731
+    assert L.dsspk_linear_bwd(stream(), B.DSSPK_BF16, p(some), K, None, p(some), N, None, 0, None, 0, 0, p(dw), None, 0, N, K, p(ws), nws) == 0
+    for part in dw.split(1 << 12):
+        assert not part.any()           # a NaN is not zero
+    del dw, ws
+    torch.cuda.empty_cache()
+
+
+def test_product_whose_copied_operand_takes_more_than_a_launch():
+    """Rows of 1023 bf16 numbers are copied to aligned ones, eight numbers a lane: 2^32 lanes for 2^25 rows.  All rows are alike but for some at either end and in the middle."""
+    M, K, N = (1 << 25) + 200, 1023, 8
+    L = B.lib()
+    nws = L.dsspk_linear_fwd_workspace_bytes(B.DSSPK_BF16, M, N, K)
+    needs(2 * M * K + nws + 4 * M * N)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")      # noqa: E731
+    w, row = (r(K, N) / 32).to(BF16), r(K).to(BF16)
+    x = torch.empty(M, K, dtype=BF16, device="cuda")
+    x[:] = row
+    places = [slice(0, 300), slice(M // 2, M // 2 + 300), slice(M - 300, M)]
+    for at in places:
+        x[at] = r(300, K).to(BF16)
+    y, ws = torch.full((M, N), float("nan"), dtype=BF16, device="cuda"), torch.empty(nws, dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()      # noqa: E731
+    assert L.dsspk_linear_fwd(stream(), B.DSSPK_BF16, p(x), K, p(w), None, 0, None, 0, p(y), N, None, 0, M, N, K, p(ws), nws) == 0
+    torch.cuda.synchronize()
+    # a sum of 1023 products in 32 bits and one rounding to 8
+    close = lambda got, a: ((got.double() - a.double() @ w.double()).abs() <= (K / 32 + 24) * 2.0 ** -23 * (a.double().abs() @ w.double().abs())       # noqa: E731
+                            + 2.0 ** -8 * (a.double() @ w.double()).abs()).all()
+    like = torch.ones(M, dtype=torch.bool, device="cuda")
+    for at in places:
+        like[at] = False
+        assert close(y[at], x[at])
+    assert close(y[1000:1001], row[None]) and (y[like] == y[1000]).all()
+    del x, y, ws
+    torch.cuda.empty_cache()

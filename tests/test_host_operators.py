@@ -47,3 +47,13 @@ def test_matrices_whose_end_passes_64_bits_are_refused(matrices):
     assert B.lib().dsspk_orthogonal_workspace_bytes(table, len(matrices)) == 0
     # refused by its arguments, in front of any launch (the addresses are never used)
     assert B.lib().dsspk_orthogonal_apply(None, 1 << 20, 2 << 20, 3 << 20, 4 << 20, 5 << 20, 100, table, len(matrices), 0.1, 0.1, 0.9, 1, 5, 1e-7, 6 << 20, 1 << 60) == -1
+
+
+@pytest.mark.parametrize("type", [0, 1])
+def test_results_of_more_tiles_than_a_launch_has_are_refused(type):
+    """by their sizes, in front of any launch (the addresses are never used)"""
+    L, at, big = B.lib(), 1 << 20, 1 << 62
+    n = 1 << 20
+    assert L.dsspk_linear_bwd(None, type, at, n, at, 2 * at, n, None, 0, None, 0, 0, 3 * at, 4 * at, 4, n, n, 5 * at, big) == -1        # dw
+    assert L.dsspk_linear_bwd(None, type, None, 0, at, 2 * at, 8, 3 * at, n, None, 0, 0, None, 4 * at, 1 << 30, 8, n, 5 * at, big) == -1       # dx
+    assert L.dsspk_linear_fwd(None, type, at, 8, 2 * at, None, 0, None, 0, 3 * at, n, None, 0, 1 << 30, n, 8, 5 * at, big) == -1
