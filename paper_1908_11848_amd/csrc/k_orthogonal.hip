@@ -743,12 +743,15 @@ extern "C" int dsspk_orthogonal_apply(void* stream, const float* w, float* w_out
     };
     for (int i = 0; i <= count; ++i) {
         const int64_t to = i < count ? matrices[i].offset : n;
-        if (to > at) {
-            if (gaps.count == GROUP) flush();
+        const int64_t most = most_blocks(256);          // of a launch; a longer gap takes several
+        while (to > at) {
+            if (gaps.count == GROUP || blocks == most) flush();
+            const int64_t room = (most - blocks) * GAP_CHUNK, end = to - at < room ? to : at + room;
             gaps.first[gaps.count] = blocks;
             gaps.from[gaps.count] = at;
-            gaps.to[gaps.count++] = to;
-            blocks += ceil_div(to - at, GAP_CHUNK);
+            gaps.to[gaps.count++] = end;
+            blocks += ceil_div(end - at, GAP_CHUNK);
+            at = end;
         }
         if (i < count) at = to + (int64_t)matrices[i].rows * matrices[i].cols;
     }

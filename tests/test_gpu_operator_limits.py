@@ -79,3 +79,22 @@ def test_product_whose_copied_operand_takes_more_than_a_launch():
     assert close(y[1000:1001], row[None]) and (y[like] == y[1000]).all()
     del x, y, ws
     torch.cuda.empty_cache()
+
+
+def test_momentum_of_more_entries_than_a_launch_takes():
+    """A vector of 2^33 entries and some beside one matrix: 2^32 threads for what is not the matrix.  Without momentum of its own and with equal gradients w' = w - rest (1 + mu) g."""
+    n, at = (1 << 33) + 1100, (1 << 33) + 1000
+    needs(3 * 4 * n)
+    w, m, g = (torch.full((n,), v, device="cuda") for v in (2.0, 0.0, 0.5))
+    table, L = B.matrix_table([(at, 4, 5)]), B.lib()
+    ws = torch.empty(L.dsspk_orthogonal_workspace_bytes(table, 1), dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()      # noqa: E731
+    assert L.dsspk_orthogonal_apply(stream(), p(w), p(w), p(m), p(m), p(g), n, table, 1, 0.5, 0.25, 0.5, 1, 5, 1e-7, p(ws), ws.numel()) == 0
+    torch.cuda.synchronize()
+    for part, value in ((w, 2.0 - 0.25 * 0.75), (m, 0.5)):
+        for i in range(0, at, 1 << 30):
+            assert (part[i:min(i + (1 << 30), at)] == value).all(), i
+        assert (part[at + 20:] == value).all()
+    assert (m[at:at + 20] == 0.5).all() and (w[at:at + 20] < 2.0).all() and (w[at:at + 20] > 1.0).all()
+    del w, m, g
+    torch.cuda.empty_cache()
