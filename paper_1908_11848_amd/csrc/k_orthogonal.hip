@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void momentum_gaps_kernel(Gaps gaps, const flo
     }
 }
 
-// u of the matrices, and the sum of squares of every chunk (squares and sums in fp64: no matrix is too large or too small for its norm)
+// u of the matrices, and the sum of squares of every chunk (squares and sums in fp64: they neither overflow nor vanish)
 template <bool NESTEROV>
 __global__ __launch_bounds__(256) void momentum_kernel(Group grp, char* ws, const float* m, float* m_out, const float* __restrict__ g, float mu) {
     __shared__ double part[4];
@@ -152,6 +152,18 @@ __device__ __forceinline__ void add_up(const Terms& t, float (&v)[8]) {
     }
 }
 
+// What u is divided by, |u| + eps, and is multiplied by first: a norm may be too large for fp32 where no entry is, and both are taken 2^-32 times then.
+struct Norm {
+    float by, norm;
+    __device__ __forceinline__ Norm() = default;
+    __device__ __forceinline__ Norm(double squares, float eps) {
+        const double d = sqrt(squares) + (double)eps;
+        by = d > 0x1p126 ? 0x1p-32f : 1.f;
+        norm = (float)(d * (double)by);
+    }
+    __device__ __forceinline__ float operator()(float u) const { return u * by / norm; }
+};
+
 // X = u / (|u| + eps) as terms, the shorter side first; 64 x 64 entries a workgroup
 __global__ __launch_bounds__(256) void normalise_kernel(Group grp, char* ws, float eps) {
     __shared__ float tile[64][65];
@@ -170,7 +182,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(Group grp, char* ws, flo
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int r = wave; r < 64; r += 4) tile[r][lane] = r0 + r < mat.rows && c0 + lane < mat.cols ? u[(long)(r0 + r) * mat.cols + c0 + lane] : 0.f;
     __syncthreads();
-    const float norm = (float)(sqrt((part[0] + part[1]) + (part[2] + part[3])) + (double)eps);
+    const Norm norm((part[0] + part[1]) + (part[2] + part[3]), eps);
     const bool turned = mat.rows > mat.cols;
     const int i0 = turned ? c0 : r0, j0 = turned ? r0 : c0;         // of X
     for (int t = threadIdx.x; t < 64 * 8; t += 256) {
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(Group grp, char* ws, flo
         if (i0 + i >= room.n || j0 + j >= room.mp) continue;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (turned ? tile[j + e][i] : tile[i][j + e]) / norm;
+        for (int e = 0; e < 8; ++e) v[e] = norm(turned ? tile[j + e][i] : tile[i][j + e]);
         write_terms(base + room.x0 + prod::terms_at(prod::terms_pitch(room.mp), i0 + i, j0 + j), v);
     }
 }
@@ -498,7 +510,7 @@ __device__ __forceinline__ void small_step(const Matrix& mat, const SmallRoom& r
     // tile t of this wavefront's share of A: rows 16 i + 4 q .., column 16 j + l16, one j for all
     const int j = wave % T;
     auto row_tile = [&](int t) { return wave / T * SQUARES + t; };
-    float norm = 0.f;
+    Norm norm;
     float4 mine[FLOATS];
     auto fetch = [&](long l0) {
         if constexpr (KIND == FIRST) {
@@ -526,7 +538,7 @@ __device__ __forceinline__ void small_step(const Matrix& mat, const SmallRoom& r
 #pragma unroll
         for (int k = 0; k < FLOATS; ++k) {
             const int t = tid + k * SMALL_THREADS, line = turned ? t / (8 * NB) : t % LINES, g = turned ? t % (8 * NB) : t / LINES;
-            L::put(xs, line, g, make_float4(mine[k].x / norm, mine[k].y / norm, mine[k].z / norm, mine[k].w / norm));
+            L::put(xs, line, g, make_float4(norm(mine[k].x), norm(mine[k].y), norm(mine[k].z), norm(mine[k].w)));
         }
     };
     fetch(begin);
@@ -540,7 +552,7 @@ __device__ __forceinline__ void small_step(const Matrix& mat, const SmallRoom& r
         __syncthreads();
         s = 0.;
         for (int i = 0; i < WAVES; ++i) s += part[i];
-        norm = (float)(sqrt(s) + (double)eps);
+        norm = Norm(s, eps);
         put();
     } else {
         // A from all stretches, in their order; B = a I + b A + c A A

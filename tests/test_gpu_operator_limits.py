@@ -98,3 +98,15 @@ def test_momentum_of_more_entries_than_a_launch_takes():
     assert (m[at:at + 20] == 0.5).all() and (w[at:at + 20] < 2.0).all() and (w[at:at + 20] > 1.0).all()
     del w, m, g
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,cols", [(33, 48), (90, 130), (130, 90)])
+def test_update_whose_norm_is_beyond_single_precision(rows, cols):
+    """Entries up to 3.3e38 fit fp32, their norm does not.  Bound: that of test_gpu_orthogonal.py, 2^-21 (3.4445^5 - 1) / 2.4445 of the result's norm."""
+    from test_gpu_orthogonal import bound, call, orthogonal
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    grad = (torch.rand(rows * cols, generator=g, device="cuda") * 2 - 1) * 3.3e38
+    w = torch.zeros_like(grad)
+    got = call(w, w, grad, [(0, rows, cols)], scale=1.0, mu=0.0)[0].double().view(rows, cols)
+    want = -orthogonal(grad.view(rows, cols), 5) * max(1, cols / rows) ** 0.5
+    assert (got - want).norm() <= bound(5) * want.norm()
