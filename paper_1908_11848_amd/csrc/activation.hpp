@@ -9,50 +9,93 @@ namespace act {
 
 constexpr float SQRT_8_OVER_PI = 1.5957691216057308f, CUBIC = 0.044715f;
 
-// e^v and 1 / v by the hardware's own instructions, a unit in the last place or so each: an epilogue over 64 million elements takes 2 us for every vector
-// instruction of an element (the library's exponential and error function take 15 and 40).
-__device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * 1.4426950408889634f); }
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-v)); }
+// Two forms of each: FINE for fp32 results, whose errors are those of a handful of fp32 roundings, and a shorter one for bf16 results, whose errors stay below 4e-7, a five
+// thousandth of what the result's rounding leaves.  An epilogue over 64 million elements takes 2 us for every vector instruction of an element (the library's exponential and
+// error function take 15 and 40).  Errors over normally distributed inputs, root mean square of the result's: see FINE and the short ones below.
 
-// The error function's part of gelu by polynomials fitted to it (largest error made small by Lawson's iteration, in 64 bits), in a = |x| up to 12, beyond which nothing
-// is left:  log2 Phi(-a), so that a Phi(-a) is off by at most 1e-7, and (Phi(-a) - a phi(a)) e^(a^2 / 2), so that the slope is off by at most 3.2e-7.
-__device__ __forceinline__ float reach(float x) { const float a = fabsf(x); return a > 12.f ? 12.f : a; }
-__device__ __forceinline__ float gelu(float x) {
-    const float a = reach(x);
-    const float l = fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(3.177492482e-05f, a, -7.569161963e-04f), a, 8.036975367e-03f), a, -5.333740498e-02f), a, -4.588343286e-01f), a,
-                              -1.151177109e+00f), a, -9.999963286e-01f);
-    return fmaf(-a, __builtin_amdgcn_exp2f(l), x < 0.f ? 0.f : x);
+// e^v and 1 / v by the hardware's own instructions, a unit in the last place or so each
+__device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * 1.4426950408889634f); }
+struct Sigmoid { float p, q; };         // sigmoid(v) and 1 - sigmoid(v)
+template <bool FINE> __device__ __forceinline__ Sigmoid sigmoid(float v) {
+    if constexpr (FINE) {
+        // of e = e^-|v| <= 1, its exponent in two parts (the product with log2 e, and what that lost); 1 / (1 + e) with a Newton step.  Neither p nor q cancels.
+        const float a = fabsf(v) > 128.f ? 128.f : fabsf(v), hi = a * -1.4426950408889634f;
+        const float lo = fmaf(a, -1.925963033500e-8f, fmaf(a, -1.4426950408889634f, -hi));
+        float e = __builtin_amdgcn_exp2f(hi);
+        e = fmaf(e, lo * 0.6931471805599453f, e);
+        const float d = 1.f + e;
+        float r = __builtin_amdgcn_rcpf(d);
+        r = fmaf(fmaf(-d, r, 1.f), r, r);
+        return v < 0.f ? Sigmoid{e * r, r} : Sigmoid{r, e * r};
+    } else {
+        const float p = __builtin_amdgcn_rcpf(1.f + exp_fast(-v));
+        return {p, 1.f - p};
+    }
 }
-__device__ __forceinline__ float gelu_slope(float x) {
-    const float a = reach(x);
-    float r = fmaf(-8.063049657e-06f, a, 1.519415503e-04f);
-    r = fmaf(fmaf(fmaf(fmaf(r, a, -1.271160005e-03f), a, 6.382798388e-03f), a, -2.223086296e-02f), a, 5.949677970e-02f);
-    r = fmaf(fmaf(fmaf(fmaf(r, a, -1.317728762e-01f), a, 2.497522908e-01f), a, -7.978648987e-01f), a, 4.999997430e-01f);
-    r *= exp_fast(-0.5f * a * a);
+
+// The error function's part of gelu by polynomials fitted to it (largest error made small by Lawson's iteration, in 64 bits) in a = |x|, up to where nothing is left.
+template <int MOST> __device__ __forceinline__ float reach(float x) { const float a = fabsf(x); return a > MOST ? (float)MOST : a; }
+// FINE: Phi(-a) e^(a^2 / 2), off by at most 2.2e-9 e^(a^2 / 2) / max(a, 1); e: e^(-a^2 / 2).  Root mean square errors 3.4e-8 of gelu and of its slope (the formula with
+// correctly rounded functions: 3.8e-8 and 4.0e-8).
+__device__ __forceinline__ float tail(float a, float& e) {
+    e = __builtin_amdgcn_exp2f(a * -0.7213475204444817f * a);
+    float r = fmaf(-7.982273337e-09f, a, 2.551311826e-07f);
+    r = fmaf(fmaf(fmaf(fmaf(r, a, -3.709441065e-06f), a, 3.280095373e-05f), a, -1.999334465e-04f), a, 9.088241295e-04f);
+    r = fmaf(fmaf(fmaf(fmaf(r, a, -3.279617335e-03f), a, 9.921597838e-03f), a, -2.627040076e-02f), a, 6.236002615e-02f);
+    r = fmaf(fmaf(fmaf(fmaf(r, a, -1.329446636e-01f), a, 2.499951506e-01f), a, -3.989420245e-01f), a, 4.999999978e-01f);
+    return r;
+}
+// short: log2 Phi(-a), so that a Phi(-a) is off by at most 1e-7, and (Phi(-a) - a phi(a)) e^(a^2 / 2), so that the slope is off by at most 3.5e-7.
+template <bool FINE> __device__ __forceinline__ float gelu(float x) {
+    if constexpr (FINE) {
+        float e;
+        const float a = reach<8>(x), r = tail(a, e);
+        return fmaf(-a, e * r, x < 0.f ? 0.f : x);
+    } else {
+        const float a = reach<12>(x);
+        const float l = fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(3.177492482e-05f, a, -7.569161963e-04f), a, 8.036975367e-03f), a, -5.333740498e-02f), a, -4.588343286e-01f), a,
+                                  -1.151177109e+00f), a, -9.999963286e-01f);
+        return fmaf(-a, __builtin_amdgcn_exp2f(l), x < 0.f ? 0.f : x);
+    }
+}
+template <bool FINE> __device__ __forceinline__ float gelu_slope(float x) {
+    float r;
+    if constexpr (FINE) {
+        float e;
+        const float a = reach<8>(x);
+        r = fmaf(a, -0.3989422804014327f, tail(a, e));
+        r *= e;
+    } else {
+        const float a = reach<12>(x);
+        r = fmaf(-8.063049657e-06f, a, 1.519415503e-04f);
+        r = fmaf(fmaf(fmaf(fmaf(r, a, -1.271160005e-03f), a, 6.382798388e-03f), a, -2.223086296e-02f), a, 5.949677970e-02f);
+        r = fmaf(fmaf(fmaf(fmaf(r, a, -1.317728762e-01f), a, 2.497522908e-01f), a, -7.978648987e-01f), a, 4.999997430e-01f);
+        r *= exp_fast(-0.5f * a * a);
+    }
     return x > 0.f ? 1.f - r : r;
 }
 
-__device__ __forceinline__ float value(int which, float x) {
+template <bool FINE> __device__ __forceinline__ float value(int which, float x) {
     switch (which) {
         case DSSPK_ACT_RELU: return x < 0.f ? 0.f : x;
-        case DSSPK_ACT_GELU: return gelu(x);
-        case DSSPK_ACT_GELU_TANH: return x * sigmoid(SQRT_8_OVER_PI * x * fmaf(CUBIC * x, x, 1.f));
-        case DSSPK_ACT_SILU: return x * sigmoid(x);
+        case DSSPK_ACT_GELU: return gelu<FINE>(x);
+        case DSSPK_ACT_GELU_TANH: return x * sigmoid<FINE>(SQRT_8_OVER_PI * x * fmaf(CUBIC * x, x, 1.f)).p;
+        case DSSPK_ACT_SILU: return x * sigmoid<FINE>(x).p;
         default: return x;
     }
 }
 
-__device__ __forceinline__ float slope(int which, float x) {
+template <bool FINE> __device__ __forceinline__ float slope(int which, float x) {
     switch (which) {
         case DSSPK_ACT_RELU: return x > 0.f ? 1.f : x == x ? 0.f : x;
-        case DSSPK_ACT_GELU: return gelu_slope(x);
+        case DSSPK_ACT_GELU: return gelu_slope<FINE>(x);
         case DSSPK_ACT_GELU_TANH: {
-            const float p = sigmoid(SQRT_8_OVER_PI * x * fmaf(CUBIC * x, x, 1.f));
-            return fmaf(x * p * (1.f - p) * SQRT_8_OVER_PI, fmaf(3.f * CUBIC * x, x, 1.f), p);
+            const Sigmoid s = sigmoid<FINE>(SQRT_8_OVER_PI * x * fmaf(CUBIC * x, x, 1.f));
+            return fmaf(x * s.p * s.q * SQRT_8_OVER_PI, fmaf(3.f * CUBIC * x, x, 1.f), s.p);
         }
         case DSSPK_ACT_SILU: {
-            const float p = sigmoid(x);
-            return p * fmaf(x, 1.f - p, 1.f);
+            const Sigmoid s = sigmoid<FINE>(x);
+            return s.p * fmaf(x, s.q, 1.f);
         }
         default: return 1.f;
     }

@@ -71,19 +71,20 @@ struct Epilogue {
 // v: eight columns of a row, n of them in the result.  SLOPE: a gradient; T: type of side and z, O: of out.
 template <bool SLOPE, class T, class O, int ACT>
 __device__ __forceinline__ void finish(const Epilogue& e, long row, int col, int n, const float (&bias)[8], const rows::Raw8<T>& side, float (&v)[8]) {
+    constexpr bool FINE = sizeof(T) == 4;
     float u[8];
     if constexpr (SLOPE) {
         if (ACT != DSSPK_ACT_NONE) {
             rows::convert8(side, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= act::slope(ACT, u[i]);
+            for (int i = 0; i < 8; ++i) v[i] *= act::slope<FINE>(ACT, u[i]);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += bias[i];
         if (e.z) rows::store8((T*)e.z + row * e.ldz + col, n, v, e.past);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act::value(ACT, v[i]);
+        for (int i = 0; i < 8; ++i) v[i] = act::value<FINE>(ACT, v[i]);
         if (e.side) {
             rows::convert8(side, u);
 #pragma unroll
