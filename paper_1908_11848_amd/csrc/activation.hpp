@@ -91,7 +91,8 @@ template <bool FINE> __device__ __forceinline__ float slope(int which, float x) 
         case DSSPK_ACT_GELU: return gelu_slope<FINE>(x);
         case DSSPK_ACT_GELU_TANH: {
             const Sigmoid s = sigmoid<FINE>(SQRT_8_OVER_PI * x * fmaf(CUBIC * x, x, 1.f));
-            return fmaf(x * s.p * s.q * SQRT_8_OVER_PI, fmaf(3.f * CUBIC * x, x, 1.f), s.p);
+            const float c = fabsf(x) > 32.f ? 32.f : x;         // there one of p and q is zero, and stays the whole term when x^2 overflows
+            return fmaf(c * s.p * s.q * SQRT_8_OVER_PI, fmaf(3.f * CUBIC * c, c, 1.f), s.p);
         }
         case DSSPK_ACT_SILU: {
             const Sigmoid s = sigmoid<FINE>(x);

@@ -67,3 +67,12 @@ def test_far_out(which):
     assert torch.equal(y[:n], x[:n]) and (y[n:2 * n].abs() <= 1e-10).all()
     assert (s[:n] == 1).all() and (s[n:2 * n].abs() <= 1e-10).all()
     assert torch.isnan(y[2 * n:]).all() and torch.isnan(s[2 * n:]).all()
+
+
+@pytest.mark.parametrize("which", CURVES)
+def test_where_squares_overflow(which):
+    """All finite numbers: the slope is 1 or 0 beyond 1e19 too, whose square fp32 does not hold."""
+    x = torch.logspace(18, 38, N // 2, device="cuda", dtype=torch.double).float()
+    s, y = slope(which, torch.cat([x, -x])), value(which, torch.cat([x, -x]))
+    assert (s[:N // 2] == 1).all() and (s[N // 2:].abs() <= 1e-10).all()
+    assert torch.equal(y[:N // 2], x) and (y[N // 2:].abs() <= 1e-10).all()
