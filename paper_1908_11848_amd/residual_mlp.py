@@ -131,11 +131,12 @@ class Training:
     """K workers of one network on one GPU, trained by a DSSP schedule (driver.Schedule)."""
 
     def __init__(self, width=256, hidden=1024, depth=2, batch=32, n_classes=10, K=4, s_L=3, r_max=12, lr=0.05, type="bf16", rule="orthogonal", matrix_lr=0.04,
-                 pool=2, config=4, device="cuda:0"):
+                 pool=2, config=4, device="cuda:0", keep=4096):
+        """keep: the losses of so many iterations of every worker stay, behind that the oldest are overwritten"""
         if type not in TYPES or rule not in ("orthogonal", "sgd"):
             raise ValueError("type is 'fp32' or 'bf16', rule 'orthogonal' or 'sgd'")
-        if not 1 <= batch <= 1024 or not 2 <= n_classes <= 1024 or min(width, hidden, K, pool) < 1 or depth < 0:
-            raise ValueError("batch in [1, 1024], n_classes in [2, 1024], width, hidden, K, pool >= 1, depth >= 0")
+        if not 1 <= batch <= 1024 or not 2 <= n_classes <= 1024 or min(width, hidden, K, pool, keep) < 1 or depth < 0:
+            raise ValueError("batch in [1, 1024], n_classes in [2, 1024], width, hidden, K, pool, keep >= 1, depth >= 0")
         self.K, self.dev = K, torch.device(device)
         torch.cuda.set_device(self.dev)
         self.seg = segments(width, hidden, depth, n_classes)
@@ -149,7 +150,7 @@ class Training:
         pitch = (n + 63) // 64 * 64
         self.w_local = torch.empty((K, pitch), dtype=torch.float32, device=self.dev)[:, :n]
         self.grad = torch.zeros((K, pitch), dtype=torch.float32, device=self.dev)[:, :n]
-        self.losses = torch.zeros((K, 4096), dtype=torch.float32, device=self.dev)         # of each worker's iterations
+        self.losses = torch.zeros((K, keep), dtype=torch.float32, device=self.dev)         # of each worker's iterations: n at n % keep
         self.steps = [Step(width, hidden, depth, batch, n_classes, type, self.dev) for _ in range(K)]
         self.streams = [torch.cuda.Stream(device=self.dev) for _ in range(K)]
         self.ctx = B.dssp_create(self.w, n, K, s_L, r_max, lr)
@@ -188,7 +189,7 @@ def main():
     for name, default in (("width", 256), ("hidden", 1024), ("depth", 2), ("batch", 32), ("workers", 4), ("pushes", 64)):
         ap.add_argument("--" + name, type=int, default=default)
     a = ap.parse_args()
-    t = Training(a.width, a.hidden, a.depth, a.batch, K=a.workers, type=a.type, rule=a.rule)
+    t = Training(a.width, a.hidden, a.depth, a.batch, K=a.workers, type=a.type, rule=a.rule, keep=a.pushes + 1)
     sched = t.schedule(inputs.durations(4, a.workers, a.pushes + 1), log=False, fused_pull=True)
     sched.advance(a.workers)            # everybody has pushed about once: first launches are not timed
     t.synchronize()
