@@ -510,6 +510,7 @@ inline bool wide(int64_t ld) { return ld > 1L << 21; }
 
 extern "C" size_t dsspk_linear_fwd_workspace_bytes(int type, int64_t M, int N, int K) {
     if (bad(type, M, N, K)) return 0;
+    if (few(type, M, N, K)) return 256;
     return pack_bytes(type, M, K) + pack_bytes(type, K, N) + partial_bytes(type, M, N, K) + 256;
 }
 

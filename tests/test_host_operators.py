@@ -57,3 +57,10 @@ def test_results_of_more_tiles_than_a_launch_has_are_refused(type):
     assert L.dsspk_linear_bwd(None, type, at, n, at, 2 * at, n, None, 0, None, 0, 0, 3 * at, 4 * at, 4, n, n, 5 * at, big) == -1        # dw
     assert L.dsspk_linear_bwd(None, type, None, 0, at, 2 * at, 8, 3 * at, n, None, 0, 0, None, 4 * at, 1 << 30, 8, n, 5 * at, big) == -1       # dx
     assert L.dsspk_linear_fwd(None, type, at, 8, 2 * at, None, 0, None, 0, 3 * at, n, None, 0, 1 << 30, n, 8, 5 * at, big) == -1
+
+
+def test_few_rows_need_no_workspace_of_the_weights_size():
+    """A row through 8192 x 8192 in fp32 takes the weights as they are, not 400 MB of terms; more rows than that way serves take the terms."""
+    f = B.lib().dsspk_linear_fwd_workspace_bytes
+    assert all(0 < f(0, m, 8192, 8192) <= 1024 for m in (0, 1, 16)) and f(0, 17, 8192, 8192) >= 6 * 8192 * 8192
+    assert all(0 < f(1, m, 4096, 1024) <= 1024 for m in (0, 1, 8)) and f(1, 9, 4096, 1024) >= 2 * 4096 * 1024
