@@ -406,6 +406,9 @@ size_t dsspk_linear_bwd_workspace_bytes(int type, int64_t M, int N, int K);
 int dsspk_linear_bwd(void* stream, int type, const void* x_dev, int64_t ldx, const void* w_dev, const void* dz_dev, int64_t lddz, void* dx_dev, int64_t lddx,
                      const void* pre_dev, int64_t ldpre, int act, float* dw_dev, float* db_dev, int64_t M, int N, int K, void* workspace_dev,
                      size_t workspace_bytes);
+/* How a product of rows x cols numbers, each a sum over K, is computed (y: M, N, K; dx: M, K, N; dw: K, N, M), for tests and measurements: rows and columns of a
+ * workgroup's tile, and in how many parts the sums are taken.  Products of few rows, which have no tiles, are not told apart.  -1: no such product. */
+int dsspk_linear_form(int type, int64_t rows, int64_t cols, int64_t K, int* tile_rows, int* tile_cols, int* parts);
 /* dst[i] = src[i] rounded to bf16 (nearest even): a worker's snapshot for products in bf16. */
 int dsspk_to_bf16(void* stream, void* dst_dev, const float* src_dev, int64_t n);
 

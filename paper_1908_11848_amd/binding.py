@@ -166,6 +166,7 @@ _SIGNATURES = {
     "dsspk_linear_bwd_workspace_bytes": (c_size_t, [c_int, c_int64, c_int, c_int]),
     "dsspk_linear_bwd": (c_int, [c_void_p, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p,
                                  c_void_p, c_int64, c_int, c_int, c_void_p, c_size_t]),
+    "dsspk_linear_form": (c_int, [c_int, c_int64, c_int64, c_int64, P(c_int), P(c_int), P(c_int)]),
     "dsspk_to_bf16": (c_int, [c_void_p, c_void_p, c_void_p, c_int64]),
     "dsspk_orthogonal_workspace_bytes": (c_size_t, [P(Matrix), c_int]),
     "dsspk_orthogonal_apply": (c_int, [c_void_p] * 6 + [c_int64, P(Matrix), c_int, c_float, c_float, c_float, c_int, c_int, c_float, c_void_p, c_size_t]),
@@ -175,6 +176,14 @@ _SIGNATURES = {
 def matrix_table(matrices):
     """[(offset, rows, cols)] of a flat vector's matrices, ascending, as the C calls take them"""
     return (Matrix * len(matrices))(*[Matrix(int(at), int(rows), int(cols)) for at, rows, cols in matrices])
+
+
+def linear_form(type, rows, cols, K):
+    """(rows and columns of a tile, parts of the reduction) that dsspk_linear_fwd and _bwd compute such a product by"""
+    out = c_int(), c_int(), c_int()
+    if lib().dsspk_linear_form(type, rows, cols, K, *[ctypes.byref(v) for v in out]):
+        raise ValueError("no product of type %d, %d x %d numbers, sums of %d" % (type, rows, cols, K))
+    return tuple(v.value for v in out)
 
 
 def lib():

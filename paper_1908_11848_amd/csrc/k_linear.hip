@@ -597,6 +597,16 @@ extern "C" int dsspk_linear_bwd(void* stream, int type, const void* x, int64_t l
     return 0;
 }
 
+extern "C" int dsspk_linear_form(int type, int64_t rows, int64_t cols, int64_t K, int* tile_rows, int* tile_cols, int* parts) {
+    if ((type != DSSPK_F32 && type != DSSPK_BF16) || rows < 1 || cols < 1 || K < 1 || rows > MAX_ROWS || cols > MAX_ROWS || K > MAX_ROWS || !tile_rows || !tile_cols || !parts) return -1;
+    if (!launchable(type, rows, cols)) return -1;
+    const Choice c = choose(type, rows, cols, K);
+    *tile_rows = COSTS[type == DSSPK_BF16][c.tile].bm;
+    *tile_cols = COSTS[type == DSSPK_BF16][c.tile].bn;
+    *parts = c.parts;
+    return 0;
+}
+
 extern "C" int dsspk_to_bf16(void* stream, void* dst, const float* src, int64_t n) {
     if (!dst || (!src && n) || n < 0 || (const void*)dst == (const void*)src || n > (1L << 40)) return -1;
     if (n == 0) return 0;

@@ -64,3 +64,15 @@ def test_few_rows_need_no_workspace_of_the_weights_size():
     f = B.lib().dsspk_linear_fwd_workspace_bytes
     assert all(0 < f(0, m, 8192, 8192) <= 1024 for m in (0, 1, 16)) and f(0, 17, 8192, 8192) >= 6 * 8192 * 8192
     assert all(0 < f(1, m, 4096, 1024) <= 1024 for m in (0, 1, 8)) and f(1, 9, 4096, 1024) >= 2 * 4096 * 1024
+
+
+def test_the_products_of_the_tests_take_every_tile_there_is():
+    import test_gpu_operator_tiles as tiles
+    assert all(B.linear_form(tiles.linear.TYPE[f[0]], *f[1:4]) == f[4] for f in tiles.FORMS)
+    one, many = ({(str(f[0]),) + f[4][:2] for f in tiles.FORMS if (f[4][2] > 1) == split} for split in (False, True))
+    large = {("torch.bfloat16", 256, 256), ("torch.float32", 128, 128), ("torch.float32", 128, 64)}
+    assert large <= one and large <= many
+    # the small tiles are what most other sizes take
+    assert B.linear_form(1, 300, 300, 72) == (128, 128, 1) and B.linear_form(0, 300, 300, 72)[:2] == (64, 64)
+    with pytest.raises(ValueError):
+        B.linear_form(0, 0, 3, 3)
