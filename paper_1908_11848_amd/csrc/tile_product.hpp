@@ -52,7 +52,7 @@ __device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigne
 
 // 16 bytes a lane from buffer + offset to LDS at `to` + 16 lane; counted by vmcnt, zero where offset + 16 passes the buffer's end
 __device__ __forceinline__ void fetch16(const intx4& buffer, unsigned offset, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(buffer) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(buffer) : "m0", "memory");
 }
 
 __device__ __forceinline__ intx4 describe(const char* p, long bytes) {
