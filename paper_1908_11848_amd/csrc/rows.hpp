@@ -34,7 +34,13 @@ template <class T> __device__ __forceinline__ void load(const T* p, int n, float
 // are read again from there (a step of a network of width 512, 8192 rows, fp32: 1450 us, 1535 past the caches).
 inline bool past_the_caches(int64_t bytes) { return bytes >= 128LL << 20; }
 // (The empty statements keep the compiler from making one store of the two branches, which would then be an ordinary one.)
-template <class V> __device__ __forceinline__ void store_past(V* p, const V& v) {
+// Not a template over the vector: that would drop the alignment of its elements from the type.
+__device__ __forceinline__ void store_past(float4u* p, const floatx4& v) {
+    asm volatile("");
+    __builtin_nontemporal_store(v, p);
+    asm volatile("");
+}
+__device__ __forceinline__ void store_past(bf16x8u* p, const bf16x8& v) {
     asm volatile("");
     __builtin_nontemporal_store(v, p);
     asm volatile("");
@@ -45,13 +51,13 @@ template <class T> __device__ __forceinline__ void store(T* p, int n, const floa
             floatx4 u;
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[e] = v[e];
-            if (past) store_past<float4u>(reinterpret_cast<float4u*>(p), u);
+            if (past) store_past(reinterpret_cast<float4u*>(p), u);
             else *reinterpret_cast<float4u*>(p) = u;
         } else {
             bf16x8 u;
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] = (bf16)v[e];
-            if (past) store_past<bf16x8u>(reinterpret_cast<bf16x8u*>(p), u);
+            if (past) store_past(reinterpret_cast<bf16x8u*>(p), u);
             else *reinterpret_cast<bf16x8u*>(p) = u;
         }
         return;
