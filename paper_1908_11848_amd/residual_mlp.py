@@ -58,7 +58,8 @@ class Step:
         self.stats = [f32(M, 2) for _ in range(depth + 1)]
         self.z, self.h = [new(M, hidden) for _ in range(depth)], [new(M, hidden) for _ in range(depth)]
         self.dx, self.dnorm, self.dh = new(M, width), new(M, width), new(M, hidden)
-        self.wide, self.dwide = f32(M, width), f32(M, width)       # the last norm's output and its gradient for the pooling
+        # the last norm's output and its gradient for the pooling, which is fp32: in fp32 they are these themselves
+        self.wide, self.dwide = (f32(M, width), f32(M, width)) if type == "bf16" else (self.norm[depth], self.dnorm)
         self.pooled, self.dpooled = f32(batch, width), f32(batch, width)
         self.logits, self.dlogits = f32(batch, n_classes), f32(batch, n_classes)
         self.copy = new(self.n) if type == "bf16" else None
@@ -72,7 +73,7 @@ class Step:
 
     def run(self, stream, x, y, w, grad, loss):
         """grad = gradient of the mean softmax cross-entropy on patches x [batch * 64][48] (of this step's type) and labels y at the fp32 weights w."""
-        with torch.cuda.stream(stream):         # for the conversions between types, which are torch copies
+        with torch.cuda.stream(stream):         # for the one conversion that is a torch copy: bf16 to fp32
             self._run(B.stream_handle(stream), x, y, w, grad, loss)
 
     def _run(self, s, x, y, w, grad, loss):
@@ -102,7 +103,9 @@ class Step:
             _ok(L.dsspk_linear_fwd(s, T, p(self.h[i]), H, mat("w2_%d" % i), vec("b2_%d" % i), B.DSSPK_ACT_NONE, p(self.x[i]), W, p(self.x[i + 1]), W, None, 0,
                                    M, W, H, ws, nws))
         norm(self.depth, "")
-        self.wide.copy_(self.norm[self.depth])
+        bf16 = T == B.DSSPK_BF16
+        if bf16:
+            self.wide.copy_(self.norm[self.depth])
         _ok(L.dsspk_gap_fwd(s, p(self.wide), p(self.pooled), self.batch, ROWS, W))
         C, m = self.n_classes, self.batch
         _ok(L.dsspk_linear_fwd(s, B.DSSPK_F32, p(self.pooled), W, vec("w_out"), vec("b_out"), B.DSSPK_ACT_NONE, None, 0, p(self.logits), C, None, 0, m, C, W, ws, nws))
@@ -110,7 +113,8 @@ class Step:
         _ok(L.dsspk_linear_bwd(s, B.DSSPK_F32, p(self.pooled), W, vec("w_out"), p(self.dlogits), C, p(self.dpooled), W, None, 0, B.DSSPK_ACT_NONE, grd("w_out"),
                                grd("b_out"), m, C, W, ws, nws))
         _ok(L.dsspk_gap_bwd(s, p(self.dpooled), p(self.dwide), m, ROWS, W))
-        self.dnorm.copy_(self.dwide)
+        if bf16:
+            _ok(L.dsspk_to_bf16(s, p(self.dnorm), p(self.dwide), self.dwide.numel()))
         norm_back(self.depth, "", self.dnorm, None)
         for i in reversed(range(self.depth)):
             # through the second product and the activation in front of it, through the first, through the norm, and past all three
