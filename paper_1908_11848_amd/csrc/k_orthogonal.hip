@@ -702,15 +702,17 @@ template <bool POLY> int steps_of_group(Group& g) {
     return deal(g, [](const Matrix& x) { const Room r(x.rows, x.cols); return (int)(lower_tiles((int)r.n) * steps_of<POLY>(r)); });
 }
 // The shares of a group's symmetric products (g.first: steps, as steps_of_group leaves it): a workgroup on every compute unit, but of eight steps (10 us) at least once half of
-// them have one, and never of less than four: joining costs as much then.  Short reductions are not cut at all where that works out without remainders: up to sixteen steps
-// take what eight and a launch that joins take (16 matrices of 256 x 1024: 350 us a call with joins, 324 without).
+// them have one, and never of less than four: joining costs as much then.  Short reductions are not cut at all where that works out without remainders.  Us a call, cut and
+// uncut: 16 matrices of 256 x 1024 346 and 320, 100 of 192 x 384 690 and 561, four of 320 x 320 287 and 255, one of 448 x 448 285 and 298, three 315 and 308.  But with twelve or
+// sixteen steps, and so few tiles that shares of four steps, which end where tiles do, leave compute units idle, they are: one matrix of 512 x 512 271 and 325, three 301 and
+// 333 (four: 358 and 329), four of 384 x 384 273 and 282 (eight: 303 and 275), AlexNet-style 395 and 415.
 template <bool POLY> Shares shares_of(const Group& g, int total, bool& whole) {
     int most = 0;
     for (int i = 0; i < g.count; ++i) {
         const int steps = steps_of<POLY>(Room(g.m[i].rows, g.m[i].cols));
         most = most > steps ? most : steps;
     }
-    whole = most <= 16;
+    whole = most <= 16 && !((most == 12 || most == 16) && total < 2 * CUS);
     for (int i = 0; i < g.count && whole; ++i) whole = g.first[i] % most == 0 && most % steps_of<POLY>(Room(g.m[i].rows, g.m[i].cols)) == 0;
     Shares s;
     s.steps = ceil_div(total, CUS);
