@@ -600,7 +600,7 @@ __device__ __forceinline__ void small_step(const Matrix& mat, const SmallRoom& r
             fetch(l0);
             if constexpr (KIND == FIRST) put();
         }
-        prod::arrived();                            // of the fetches too
+        prod::arrived();                            // the lines are there, by fetches or by put()
         if constexpr (KIND != FIRST) {
             // a wavefront's own 16 lines: rows of a result tile are the short side, columns the lines
             static_assert(LINES == 16 * WAVES, "");
@@ -634,7 +634,6 @@ __device__ __forceinline__ void small_step(const Matrix& mat, const SmallRoom& r
             if constexpr (KIND != LAST) __syncthreads();
         }
         if constexpr (KIND != LAST) {
-            if constexpr (KIND == FIRST) __syncthreads();
 #pragma unroll
             for (int k = 0; k < COPIES; ++k) {
                 const int at = (k * SMALL_THREADS + tid) * 16;
@@ -694,8 +693,6 @@ template <class F> int deal(Group& g, F of) {
     return blocks;
 }
 
-}  // namespace
-
 constexpr int CUS = 256;
 template <bool V> struct Set { static constexpr bool value = V; };
 template <bool POLY> int steps_of_group(Group& g) {
@@ -722,6 +719,8 @@ template <bool POLY> Shares shares_of(const Group& g, int total, bool& whole) {
     return s;
 }
 constexpr size_t PARTIAL_BYTES = 2 * (size_t)CUS * TILE_FLOATS * 4;
+
+}  // namespace
 
 extern "C" size_t dsspk_orthogonal_workspace_bytes(const dsspk_matrix* matrices, int count) {
     if (bad(matrices, count)) return 0;
