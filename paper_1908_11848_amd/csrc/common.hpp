@@ -9,9 +9,6 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 static inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
-// The most workgroups of so many threads that a launch takes: HIP refuses 2^32 threads or more in a dimension.
-static inline long most_blocks(int threads) { return (1L << 31) / threads; }
-
 // Number of workgroups that keeps every CU of the chip busy a few times over for a
 // bandwidth-bound grid-stride kernel (256 CUs in 8 XCDs; workgroups are dealt to XCDs
 // round-robin, so a multiple of 8 keeps the XCDs evenly loaded).

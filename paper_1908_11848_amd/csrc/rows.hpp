@@ -3,6 +3,9 @@
 #pragma once
 #include "common.hpp"
 
+// The most workgroups of so many threads that a launch takes: one of 2^32 threads or more in a dimension is cut short without an error.
+inline long most_blocks(int threads) { return (1L << 31) / threads; }
+
 namespace rows {
 
 typedef __bf16 bf16;
