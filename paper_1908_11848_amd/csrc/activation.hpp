@@ -9,9 +9,9 @@ namespace act {
 
 constexpr float SQRT_8_OVER_PI = 1.5957691216057308f, CUBIC = 0.044715f;
 
-// Two forms of each: FINE for fp32 results, whose errors are those of a handful of fp32 roundings, and a shorter one for bf16 results, whose errors stay below 4e-7, a five
-// thousandth of what the result's rounding leaves.  An epilogue over 64 million elements takes 2 us for every vector instruction of an element (the library's exponential and
-// error function take 15 and 40).  Errors over normally distributed inputs, root mean square of the result's: see FINE and the short ones below.
+// Two forms of each: FINE for fp32 results, whose errors are those of a handful of fp32 roundings (2^-24 of the results' root mean square), and a shorter one for bf16 results, whose
+// errors, 1.4e-6 at most where the value is about 1 (the slope of gelu's tanh form), are a thousandth of what rounding to bf16 leaves.  An epilogue over 64 million elements takes 2 us for
+// every vector instruction of an element (the library's exponential and error function take 15 and 40).
 
 // e^v and 1 / v by the hardware's own instructions, a unit in the last place or so each
 __device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * 1.4426950408889634f); }

@@ -3,8 +3,8 @@
 // Both are bound by memory: forward reads and writes a row once (2 x C elements), backward reads x and dy (and the shortcut's gradient) and writes dx. So
 // a row stays in registers between its sums and its result: mean, then the squares of the deviations from it (two passes over
 // registers, one over memory), everything in fp32.  WAVES wavefronts share a row, a lane holds E elements of it in vectors of 16 bytes.
-// Measured: forward 16384 x 1024 fp32 20.7 us (6.5 TB/s), 65536 x 2048 bf16 85 us (6.3); backward 65536 x 2048 bf16 with a shortcut 200 us (5.4; a copy of 1 GB runs at 5.1),
-// 16384 x 1024 fp32 45 us (6.0).  Rows of more than 8192 channels backward run at half that: no registers are left to fetch ahead.
+// Measured: forward 16384 x 1024 fp32 20.8 us in the kernel (6.4 TB/s: part of it comes out of the last cache), 25.5 a call; backward 65536 x 2048 bf16 with a shortcut 192 us and 5.5 for the sums, 201 a
+// call (5.4 TB/s; a copy of 1 GB runs at 5.0 to 5.1).  Rows of more than 8192 channels backward run at half that: no registers are left to fetch ahead.
 //
 // The weights' gradients are sums over rows.  A workgroup takes every G-th group of rows, and as a lane's channels stay the same, adds
 // its share up in registers; G records of 2 C sums go to scratch memory and are added up by a second kernel in the order of their number.  No atomics: the

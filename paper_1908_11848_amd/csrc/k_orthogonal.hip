@@ -11,8 +11,8 @@
 // Matrices with a short side of at most DSSPK_ORTHOGONAL_SMALL go through a step in one launch: a workgroup holds a stretch of X in LDS, works out B for itself from the
 // partial sums of A that all stretches left behind, multiplies, and leaves its own share of the next A.
 //
-// Measured (us a call, 5 steps): four matrices of 1024 x 4096 and four of 4096 x 1024 3380 (a step: A 208 + 16, B 66 + 23, X 382; X at 1.08 PFLOP/s in bf16), ResNet-110's 109 filters 101 (a launch
-// a step: 16), AlexNet-style 415: 3136 x 384 and 384 x 192 in launches of 12 to 26 that few compute units have a part in.
+// Measured (us a call, 5 steps): four matrices of 1024 x 4096 and four of 4096 x 1024 3340 to 3400 (a step: A 199 + 16, B 62 + 23, X 361; X at 1.14 PFLOP/s in bf16), ResNet-110's 109 filters 101 (a
+// launch a step: 15.5), AlexNet-style 395: 3136 x 384 and 384 x 192 in launches of 11 to 14 that few compute units have a part in.
 #include "rows.hpp"
 #include "tile_product.hpp"
 #include "../../include/dssp_kernels.h"

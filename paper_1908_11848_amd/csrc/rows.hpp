@@ -33,8 +33,9 @@ template <class T> __device__ __forceinline__ void load(const T* p, int n, float
     for (int e = 0; e < VEC<T>; ++e) v[e] = e < n ? (float)p[e] : 0.f;
 }
 // Results of more than half of the last cache are written past the caches: what is next to read them finds nothing of them there anyway, and what the kernel reads
-// stays (layer norm forward, 65536 x 2048 bf16, 109 us without that and 85 with it; a product's epilogue that reads as much as it writes, 134 MB, 188 and 172).  Smaller ones
-// are read again from there (a step of a network of width 512, 8192 rows, fp32: 1450 us, 1535 past the caches).
+// stays.  A block's forward pass (layer norm, product with GELU, product with residual; bf16, the hidden layer's results of 128 to 224 MB read by the next product) takes 295, 432, 501 and 561 us so and
+// 338, 449, 518 and 585 with the caches up to 256 MB, its backward pass 646, 808, 930 and 1068 and 658, 819, 945 and 1078; of eight such blocks none was slower.  Smaller results are read again
+// from there (a step of a network of width 512, 8192 rows, fp32: 1450 us, 1535 past the caches).
 inline bool past_the_caches(int64_t bytes) { return bytes >= 128LL << 20; }
 // (The empty statements keep the compiler from making one store of the two branches, which would then be an ordinary one.)
 // Not a template over the vector: that would drop the alignment of its elements from the type.

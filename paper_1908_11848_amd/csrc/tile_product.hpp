@@ -19,9 +19,10 @@
 //
 // The matrix-core tile is transposed: its rows are C's columns, so that a lane holds four consecutive columns of one row of C.
 //
-// Measured, 4096 x 4096 x 4096 bf16: 102 us, 1.35 PFLOP/s with 256 x 256 tiles (a library product of 8192 cubed runs at 1.25 on this chip), 126 us with 128 x 128; three
-// planes, 4096 x 4096 x 1024: 153 us, 225 TFLOP/s of fp32 (the library's fp32 150), 1.35 PFLOP/s in bf16.  Bound by the matrix cores and their clock under load: busy 65 to 70 % of the
-// cycles in the kernels of three planes, 55 in a split bf16 one; LDS is active in a quarter of them, without conflicts.
+// Measured, whole calls of a forward product: bf16 4096 x 4096 x 4096 117 to 127 us, 8192 cubed 751 to 804 us, 1.37 to 1.46 PFLOP/s (the library 795 to 890); three planes, 4096 x 4096 x 4096 633
+// to 639 us, 217 TFLOP/s of fp32, 1.3 PFLOP/s in bf16 (the library's fp32 125 to 133 TFLOP/s).  Bound by the matrix cores and their clock under load: busy 55 to 70 % of the cycles in the
+// kernels of three planes, but 25 with the 64 x 64 tile; of one plane 57 in a split product, 32 and 42 where an epilogue follows.  LDS is active in 15 to 27 % of them, with conflicts in 0 to 3 % of
+// those, 9 where the last step of an update turns its results round in LDS and 33 with the 64 x 64 tile of three planes, whose KO rows have 24 chunks; why was not followed up.
 #pragma once
 #include "split.hpp"
 
