@@ -393,7 +393,8 @@ int dsspk_layernorm_bwd(void* stream, int type, const void* x_dev, int64_t ldx, 
 
 /* y[M][N] = act(x[M][K] w[K][N] + bias) + residual, sums, bias, activation and residual in fp32, one rounding.  w_dev is contiguous.  bias_dev, residual_dev
  * NULL: none.  z_dev (NULL: not wanted) receives x w + bias, which the activation's gradient needs.  residual_dev may be y_dev (ldr = ldy).  DSSPK_F32: fp32
- * products as three bf16 terms on the bf16 matrix cores, over all of fp32's range, as the 3x3 convolutions have them.  workspace_dev:
+ * products as three bf16 terms on the bf16 matrix cores, over all of fp32's range, as the 3x3 convolutions have them; activations and slopes to a few fp32 roundings (in
+ * bf16 calls to 2^-19 of the larger of the value and 1, in front of the rounding to 8 bits).  workspace_dev:
  * dsspk_linear_fwd_workspace_bytes(...) bytes, 256-byte aligned.  M = 0 does nothing; K, N >= 1, at most 2^20 each, M at most 2^30, rows at most 2^21 elements apart; results
  * (y, dx, dw) whose tiles are more than a launch has workgroups, which begins beyond 2^35 numbers, are refused. */
 size_t dsspk_linear_fwd_workspace_bytes(int type, int64_t M, int N, int K);
